@@ -149,12 +149,12 @@ class Explainer:
         out[..., M] = self.bias
         return out
 
-
     def server(self, rows: int):
         """A function that explains batches of exactly `rows` rows, as ``explain`` does, by
         replaying a HIP graph of its launches: a few rows take the device less time than the
         host needs to enqueue them.  The result is overwritten by the next call.  The graph
-        reads the network's weights where they are, so it follows further training."""
+        reads the network's weights where they are, so it follows further training; the
+        function keeps them, also where the network itself is dropped."""
         X = torch.zeros(rows, self.shape[1], device=self.X.device)
         side = torch.cuda.Stream()
         side.wait_stream(torch.cuda.current_stream())
@@ -171,6 +171,8 @@ class Explainer:
             X.copy_(batch)
             graph.replay()
             return out
+        # the graph holds addresses alone: its inputs live as long as the function
+        explain.reads = (*self.weights.values(), self.mean, self.dev, self.bias)
         return explain
 
 
