@@ -11,7 +11,10 @@ for a row it then runs the network alone.
     h -> W_out -> the values of every output, in units of their spread
 
 Weights are float32; the products take bfloat16 copies that the optimizer's step
-writes.  The bias column is the ensemble's own.
+writes.  The bias column is the ensemble's own.  In float16, whose numbers end at 6e-8 and
+65504, the backward pass runs on scaled gradients: those of the mean over 4096 rows of 784
+values are below the least number otherwise.  The optimizer takes the scale off again, in
+32 bits; gradients that overflow change nothing but the scale, which is halved.
 
     python -m paper_2010_13972_amd.explainer --workload covtype_med --steps 400
 """
@@ -24,6 +27,9 @@ import torch
 
 from . import gts, nn
 
+# In float16, the gradient of a value starts at this times its error: sums over some 1e5
+# rows stay finite, and errors down to 1e-3 of the values' spread keep all their bits.
+_SCALE = 0.125
 _BLOCK = ("w_g", "b_g", "w_1", "b_1", "w_2", "b_2", "w_post", "w_pre", "scale")
 
 
@@ -64,6 +70,7 @@ class Explainer:
         self.weights = dict(zip(self.names, tensors if self.copies is None else self.copies))
         self.state = nn.adamw_state(tensors, state_bits)
         self.step_number = 0
+        self.loss_scale = torch.full((), _SCALE, device=X.device) if dtype == torch.float16 else None
 
     def _inputs(self, X):
         return ((X - self.mean) / self.dev).to(self.dtype)
@@ -119,14 +126,31 @@ class Explainer:
         want = self.targets(X)
         y, kept = self.forward(X, keep=True)
         off = y.float() - want
-        g = self.backward((off * (2.0 / off.numel())).to(self.dtype), kept)
+        mean = 2.0 / off.numel()
+        dy = off * (mean if self.loss_scale is None else self.loss_scale)
+        g = self.backward(dy.to(self.dtype), kept)
         grads = [g[n] for n in self.names]
+        clip = nn.grad_clip(grads, max_norm)
+        if self.loss_scale is not None:
+            clip = self._unscale(clip, mean, max_norm)
         self.step_number += 1
         s = self.state
         nn.adamw_step(self.master, grads, s.m, s.v, m_scale=s.m_scale, v_scale=s.v_scale,
-                      copies=self.copies, clip=nn.grad_clip(grads, max_norm),
-                      step=self.step_number, lr=lr, weight_decay=0.01)
+                      copies=self.copies, clip=clip, step=self.step_number, lr=lr,
+                      weight_decay=0.01)
         return off.square().mean()
+
+    def _unscale(self, clip, mean: float, max_norm: float):
+        """grad_clip's result for the gradients as they are, from that of the scaled ones: the
+        factor takes the scale off too.  Moves the scale: half after an overflow, then back
+        by a thousandth a step."""
+        s = self.loss_scale
+        undo = mean / s
+        norm = clip[0] * undo
+        there = torch.isfinite(norm)
+        factor = torch.where(there, (max_norm / (norm + 1e-6)).clamp(max=1.0) * undo, float("nan"))
+        s.copy_(torch.where(there, s * 1.001, s * 0.5).clamp(2.0 ** -20, _SCALE))
+        return torch.stack([norm, factor])
 
     def fit(self, steps: int, rows: int = 4096, lr: float = 1e-3, seed: int = 0, report=None):
         """Trains on `steps` batches of rows drawn from X.  report(step, loss): every 50th."""
