@@ -45,7 +45,10 @@ class Explainer:
         phi = gts.shap(model, X[:1024])
         self.bias = phi[0, :, -1].float()
         self.spread = float(phi[..., :-1].float().std()) or 1.0
-        self.mean, self.dev = X.mean(0), X.std(0).clamp_min(1e-6)
+        # a feature that never varied keeps its unit: rows explained later may have other values
+        same = (X == X[0]).all(0)
+        self.mean = torch.where(same, X[0], X.mean(0))
+        self.dev = torch.where(same, 1.0, X.std(0, correction=min(1, X.shape[0] - 1)).clamp_min(1e-6))
         g = torch.Generator(device=X.device).manual_seed(seed)
         m, outs = model.num_features, model.num_groups * model.num_features
 
