@@ -44,7 +44,8 @@ class Explainer:
         self.X = X
         phi = gts.shap(model, X[:1024])
         self.bias = phi[0, :, -1].float()
-        self.spread = float(phi[..., :-1].float().std()) or 1.0
+        values = phi[..., :-1].float()
+        self.spread = float(values.std(correction=min(1, values.numel() - 1))) or 1.0
         # a feature that never varied keeps its unit: rows explained later may have other values
         same = (X == X[0]).all(0)
         self.mean = torch.where(same, X[0], X.mean(0))

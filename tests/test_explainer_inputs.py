@@ -1,4 +1,4 @@
-"""How an explainer network scales its inputs, without a GPU: the exact values
+"""How an explainer network scales its inputs and values, without a GPU: the exact values
 are stood in for."""
 import warnings
 from types import SimpleNamespace
@@ -35,3 +35,10 @@ def test_a_feature_without_variation_keeps_its_unit(monkeypatch, value):
 def test_one_row(monkeypatch):
     net = network(monkeypatch, torch.randn(1, 3))
     assert torch.equal(net._inputs(net.X), torch.zeros(1, 3)) and net.spread > 0
+
+
+@pytest.mark.parametrize("values", [lambda rows: torch.ones(rows, 1, 2), lambda rows: torch.zeros(rows, 1, 2)])
+def test_one_value(monkeypatch, values):
+    """One feature and one row have no spread; neither have values that are all alike."""
+    assert network(monkeypatch, torch.randn(1, 1), values=values).spread == 1.0
+    assert network(monkeypatch, torch.randn(5, 1), values=values).spread == 1.0
