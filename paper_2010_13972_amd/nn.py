@@ -234,7 +234,7 @@ def linear(x, weight, bias=None, *, residual=None, act="none", save_pre=False, o
     if residual is not None:
         a.residual, a.ld_r = _matrix("residual", residual, rows, outputs, dtype, dev)
     size = 4 if a.dtype == 0 else 2
-    aligned = rows > 0 and _lie(a.x | a.w, (a.ld_x | a.ld_w) * size)
+    aligned = rows * inputs * outputs > 0 and _lie(a.x | a.w, (a.ld_x | a.ld_w) * size)
     need = _need("gts_linear_workspace_bytes", rows, inputs, outputs, a.dtype, aligned)
     pre = None
     with _on(stream):
@@ -280,7 +280,8 @@ def linear_backward(dy, x, weight, *, pre=None, act="none", bias=True, dx=True, 
             raise ValueError(f"act {act!r} needs pre")
         a.pre, a.ld_pre = _matrix("pre", pre, rows, outputs, dtype, dev)
     size = 4 if a.dtype == 0 else 2
-    aligned = rows > 0 and _lie(a.dy | a.x | a.w, (a.ld_dy | a.ld_x | a.ld_w) * size)
+    aligned = (rows * inputs * outputs > 0 and
+               _lie(a.dy | a.x | a.w, (a.ld_dy | a.ld_x | a.ld_w) * size))
     need = _need("gts_linear_backward_workspace_bytes", rows, inputs, outputs, a.dtype, aligned)
     gx = gw = gb = None
     with _on(stream):
