@@ -441,6 +441,8 @@ extern "C" gts_status gts_linear_backward(const gts_linear_grad_args* a, void* d
   const bool products = a->dx != nullptr || a->dw != nullptr;
   const bool direct = lies(a->dy, a->ld_dy, es) && (a->dx == nullptr || a->outputs * es % 16 == 0);
   const bool make = products && (a->act != GTS_ACT_NONE || !direct);
+  // the products read dz where it lies: a bad address is refused before it is planned with
+  if (make && (st = check_workspace(d_workspace, workspace_bytes, l.product)) != GTS_OK) return st;
   ProductArgs px{}, pw{};
   px.a = make ? d_workspace : a->dy;
   px.lda = make ? l.ld_dz : a->ld_dy;
