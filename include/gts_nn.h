@@ -157,7 +157,7 @@ gts_status gts_linear_backward(const gts_linear_grad_args *args, void *d_workspa
  * w_post, w_pre  [width].
  * u, h    [rows][width], overwritten; u may be x itself, h may be f itself (same
  *         pointer and stride).
- * width is at most GTS_NORM_MAX_WIDTH.  Errors as for gts_linear.
+ * width is at most GTS_NORM_MAX_WIDTH, eps 0 or more.  Errors as for gts_linear.
  */
 typedef enum gts_norm { GTS_NORM_RMS = 0, GTS_NORM_LAYER = 1 } gts_norm;
 typedef enum gts_gate { GTS_GATE_NONE = 0, GTS_GATE_LINEAR = 1, GTS_GATE_SIGMOID = 2 } gts_gate;

@@ -426,7 +426,7 @@ int64_t grad_groups(int64_t rows, int64_t width, int64_t size) {
   return std::min(ceil_div(rows, at_once * 2), most);
 }
 
-gts_status check_norm(int64_t rows, int64_t width, int32_t dtype, int32_t norm, int32_t gate_act) {
+gts_status check_norm(int64_t rows, int64_t width, int32_t dtype, int32_t norm, int32_t gate_act, float eps) {
   if (!known_type(dtype)) return fail(GTS_EINVAL, "dtype %d is not GTS_F32, GTS_BF16 or GTS_F16", dtype);
   if (rows < 0 || rows > INT32_MAX) return fail(GTS_EINVAL, "rows must be >= 0 and below 2^31");
   if (width < 1 || width > GTS_NORM_MAX_WIDTH)
@@ -434,6 +434,7 @@ gts_status check_norm(int64_t rows, int64_t width, int32_t dtype, int32_t norm, 
   if (norm != GTS_NORM_RMS && norm != GTS_NORM_LAYER) return fail(GTS_EINVAL, "unknown norm %d", norm);
   if (gate_act < GTS_GATE_NONE || gate_act > GTS_GATE_SIGMOID)
     return fail(GTS_EINVAL, "unknown gate %d", gate_act);
+  if (!(eps >= 0.0f)) return fail(GTS_EINVAL, "eps must be >= 0");
   return GTS_OK;
 }
 
@@ -450,7 +451,7 @@ extern "C" gts_status gts_norm_residual(const gts_norm_args* a, void* stream) {
   using namespace gts::nn;
   clear_error();
   if (a == nullptr) return fail(GTS_EINVAL, "args must not be NULL");
-  gts_status st = check_norm(a->rows, a->width, a->dtype, a->norm, a->gate_act);
+  gts_status st = check_norm(a->rows, a->width, a->dtype, a->norm, a->gate_act, a->eps);
   if (st != GTS_OK) return st;
   const bool gated = a->gate_act != GTS_GATE_NONE;
   if (!gated && a->gate != nullptr) return fail(GTS_EINVAL, "a gate without a gate_act");
@@ -487,7 +488,7 @@ extern "C" gts_status gts_norm_residual_backward_workspace_bytes(int64_t rows, i
   using namespace gts;
   clear_error();
   if (bytes == nullptr) return fail(GTS_EINVAL, "bytes must not be NULL");
-  gts_status st = nn::check_norm(rows, width, GTS_F32, GTS_NORM_RMS, GTS_GATE_NONE);
+  gts_status st = nn::check_norm(rows, width, GTS_F32, GTS_NORM_RMS, GTS_GATE_NONE, 0.0f);
   if (st != GTS_OK) return st;
   const int64_t groups = std::max(nn::grad_groups(rows, width, 2), nn::grad_groups(rows, width, 4));
   *bytes = nn::ceil_div(groups * 3 * width * 4, 16) * 16;
@@ -500,7 +501,7 @@ extern "C" gts_status gts_norm_residual_backward(const gts_norm_grad_args* a, vo
   using namespace gts::nn;
   clear_error();
   if (a == nullptr) return fail(GTS_EINVAL, "args must not be NULL");
-  gts_status st = check_norm(a->rows, a->width, a->dtype, a->norm, a->gate_act);
+  gts_status st = check_norm(a->rows, a->width, a->dtype, a->norm, a->gate_act, a->eps);
   if (st != GTS_OK) return st;
   const bool gated = a->gate_act != GTS_GATE_NONE;
   const bool empty = a->rows == 0;
