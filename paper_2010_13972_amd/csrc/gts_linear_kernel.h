@@ -151,10 +151,12 @@ __device__ __forceinline__ void copy_to_lds(const char* lds, u32x4 buffer, unsig
 #ifdef __HIP_DEVICE_COMPILE__
   const auto to = GTS_LDS(const_cast<char*>(lds));
   if constexpr (WRITTEN) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+    // the buffer's registers may have been written by a vector instruction just before, which
+    // a load has to stand 5 wait states behind; the compiler does not count them in here
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                  :
                  : "s"(scalar((uint32_t)reinterpret_cast<uintptr_t>(to))), "v"(at), "s"(buffer)
-                 : "memory");
+                 : "memory", "m0");
   } else {
     void* base = reinterpret_cast<void*>((uint64_t)buffer[1] << 32 | buffer[0]);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(base, 0, (int)buffer[2], (int)buffer[3]),
