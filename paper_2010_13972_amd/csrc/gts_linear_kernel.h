@@ -716,6 +716,22 @@ __global__ __launch_bounds__(256) void join_kernel(const ProductArgs p) {
   finish<T, 1, 4>(p, m, n, bias, z);
 }
 
+// What thread `i` of a copy takes: 16 bytes of operand a, whose pieces come first, or of b.
+struct AlignPiece {
+  bool there, second;
+  int64_t row, col;
+};
+template <int E>
+__host__ __device__ __forceinline__ AlignPiece align_piece(const AlignArgs& a, const AlignArgs& b, int64_t pieces_a,
+                                                           int64_t i) {
+  const bool second = i >= pieces_a;
+  const AlignArgs& o = second ? b : a;
+  if (o.dst == nullptr) return {false, second, 0, 0};   // its rows have no length to divide by
+  if (second) i -= pieces_a;
+  const int64_t pieces = o.ld_dst / E, row = i / pieces, col = i % pieces * E;
+  return {row < o.rows, second, row, col};
+}
+
 // Copies up to two operands; a thread copies 16 bytes.  1000 x 2048 in fp16 from a slice of
 // rows 2053 apart takes 5.0 us, a launch's latency among them; the product of it and 785
 // outputs 18.7 in all, and 22.1 through registers, which need no copy (256 x 54 x 512 in
@@ -723,11 +739,10 @@ __global__ __launch_bounds__(256) void join_kernel(const ProductArgs p) {
 template <class T>
 __global__ __launch_bounds__(256) void align_kernel(const AlignArgs a, const AlignArgs b, int64_t pieces_a) {
   constexpr int E = kVec<T>;
-  int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const AlignArgs& o = i < pieces_a ? a : b;
-  if (i >= pieces_a) i -= pieces_a;
-  const int64_t pieces = o.ld_dst / E, row = i / pieces, col = i % pieces * E;
-  if (o.dst == nullptr || row >= o.rows) return;
+  const AlignPiece piece = align_piece<E>(a, b, pieces_a, (int64_t)blockIdx.x * 256 + threadIdx.x);
+  if (!piece.there) return;
+  const AlignArgs& o = piece.second ? b : a;
+  const int64_t row = piece.row, col = piece.col;
   const T* from = static_cast<const T*>(o.src) + row * o.ld + col;
   typename Fragment<T>::type v;
   if (o.width - col >= E) {
