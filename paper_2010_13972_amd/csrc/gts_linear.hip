@@ -246,7 +246,7 @@ __global__ __launch_bounds__(256) void dz_kernel(const T* dy, int64_t ld_dy, con
 template <class T>
 __global__ __launch_bounds__(1024) void column_sum_kernel(const float* sums, int64_t chunks,
                                                           int64_t n, T* out) {
-  const int64_t c = (int64_t)blockIdx.x * kSumColumns + threadIdx.x % kSumColumns;
+  const int64_t c = group_of_grid() * kSumColumns + threadIdx.x % kSumColumns;
   const float sum = column_sum<1024>(sums, chunks, n, c);
   if (threadIdx.x < kSumColumns && c < n) out[c] = (T)sum;
 }
@@ -481,7 +481,7 @@ extern "C" gts_status gts_linear_backward(const gts_linear_grad_args* a, void* d
       return check_launch(e);
     }
     if (e == hipSuccess && a->db) {
-      column_sum_kernel<T><<<(unsigned)ceil_div(a->outputs, kSumColumns), 1024, 0, s>>>(
+      column_sum_kernel<T><<<grid_of(ceil_div(a->outputs, kSumColumns)), 1024, 0, s>>>(
           sums, l.dz.chunks, a->outputs, static_cast<T*>(a->db));
       e = hipGetLastError();
     }

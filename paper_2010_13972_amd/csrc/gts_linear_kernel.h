@@ -80,8 +80,6 @@ hipError_t launch_pair_bf16(const ProductArgs& x, const ProductArgs& w, int shap
 hipError_t launch_pair_f16(const ProductArgs& x, const ProductArgs& w, int shape, const AlignArgs& align_w,
                            const AlignArgs& align_x, const ColumnSums& sums, hipStream_t s);
 
-constexpr int64_t kMostItems = ((int64_t)1 << 32) - 1;   // work-items of a launch
-
 constexpr int kSliceBytes = 128;   // depth of a slice, in bytes of k
 template <class T>
 constexpr int kDepth = kSliceBytes / (int)sizeof(T);
@@ -321,6 +319,10 @@ __device__ __forceinline__ void barrier() {
   pin();
   __builtin_amdgcn_s_barrier();
   pin();
+}
+
+__device__ __forceinline__ unsigned tile_count(const ProductArgs& p) {
+  return (unsigned)p.tiles_m * (unsigned)p.tiles_n * (unsigned)p.splits;
 }
 
 // The tile that workgroup `id` of `count` takes.  Workgroups go round the 8 XCDs, each
@@ -566,7 +568,8 @@ __device__ __forceinline__ void product_tile(const ProductArgs& p, unsigned id, 
 template <class T, int L, int S, bool DIRECT>
 __global__ __launch_bounds__(kTileThreads<S>, TileShape<S>::OCC) void product_kernel(const ProductArgs p) {
   __shared__ __attribute__((aligned(1024))) char lds[kTileLds<S, DIRECT>];
-  product_tile<T, L, S, DIRECT>(p, blockIdx.x, gridDim.x, lds);
+  const unsigned id = (unsigned)group_of_grid(), count = tile_count(p);
+  if (id < count) product_tile<T, L, S, DIRECT>(p, id, count, lds);
 }
 
 // Both gradient products and the bias' sums in one launch, for products of small tiles:
@@ -611,7 +614,9 @@ __global__ __launch_bounds__(512, 2) void large_kernel(const ProductArgs p) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
   const int wm = wave / 4 * (FM * 16), wn = wave % 4 * (FN * 16);
   int tm, tn, split;
-  tile_of(p, blockIdx.x, gridDim.x, tm, tn, split);
+  const unsigned id = (unsigned)group_of_grid(), count = tile_count(p);
+  if (id >= count) return;
+  tile_of(p, id, count, tm, tn, split);
   const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
   const int64_t k0 = split * p.k_chunk, end = min(p.k, k0 + p.k_chunk);
   const int slices = __builtin_amdgcn_readfirstlane((int)ceil_div(end - k0, (int64_t)D));
@@ -690,7 +695,7 @@ __global__ __launch_bounds__(512, 2) void large_kernel(const ProductArgs p) {
 template <class T>
 __global__ __launch_bounds__(256) void join_kernel(const ProductArgs p) {
   const int64_t quads = (p.n + 3) / 4;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t i = group_of_grid() * 256 + threadIdx.x;
   if (i >= p.m * quads) return;
   constexpr int AHEAD = 4;
   const int64_t m[1] = {i / quads}, n = i % quads * 4;
@@ -739,7 +744,7 @@ __host__ __device__ __forceinline__ AlignPiece align_piece(const AlignArgs& a, c
 template <class T>
 __global__ __launch_bounds__(256) void align_kernel(const AlignArgs a, const AlignArgs b, int64_t pieces_a) {
   constexpr int E = kVec<T>;
-  const AlignPiece piece = align_piece<E>(a, b, pieces_a, (int64_t)blockIdx.x * 256 + threadIdx.x);
+  const AlignPiece piece = align_piece<E>(a, b, pieces_a, group_of_grid() * 256 + threadIdx.x);
   if (!piece.there) return;
   const AlignArgs& o = piece.second ? b : a;
   const int64_t row = piece.row, col = piece.col;
@@ -764,7 +769,8 @@ __global__ __launch_bounds__(512) void few_rows_kernel(const ProductArgs p) {
   typedef typename Fragment<T>::type Piece;
   __shared__ f32x4 sums[WAVES][RB][64];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int64_t n0 = group_of_grid() * 16;
+  if (n0 >= p.n) return;
   const int64_t steps = ceil_div(p.k, STEP), each = ceil_div(steps, WAVES);
   const int64_t first = wave * each, last = min(steps, first + each);
   // lane i of 16 takes row i of W (of x), the 16-byte piece lane / 16 of a step
@@ -815,7 +821,7 @@ __global__ __launch_bounds__(512) void few_rows_kernel(const ProductArgs p) {
 }
 
 inline hipError_t launch_join(const ProductArgs& p, hipStream_t s, void (*kernel)(ProductArgs)) {
-  kernel<<<(unsigned)ceil_div(p.m * ceil_div(p.n, 4), 256), 256, 0, s>>>(p);
+  kernel<<<grid_of(ceil_div(p.m * ceil_div(p.n, 4), 256)), 256, 0, s>>>(p);
   return hipGetLastError();
 }
 
@@ -825,8 +831,8 @@ hipError_t launch_tiles(ProductArgs p, hipStream_t s) {
   p.tiles_m = (int32_t)ceil_div(p.m, Sh::BM);
   p.tiles_n = (int32_t)ceil_div(p.n, Sh::BN);
   const int64_t groups = (int64_t)p.tiles_m * p.tiles_n * p.splits;
-  if (groups > kMostItems / 512) return hipErrorInvalidValue;
-  product_kernel<T, L, S, DIRECT><<<(unsigned)groups, kTileThreads<S>, 0, s>>>(p);
+  if (groups > INT32_MAX) return hipErrorInvalidValue;   // larger than any memory
+  product_kernel<T, L, S, DIRECT><<<grid_of(groups), kTileThreads<S>, 0, s>>>(p);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess && p.splits > 1 ? launch_join(p, s, join_kernel<T>) : e;
 }
@@ -836,8 +842,8 @@ hipError_t launch_large(ProductArgs p, hipStream_t s) {
   p.tiles_m = (int32_t)ceil_div(p.m, BM);
   p.tiles_n = (int32_t)ceil_div(p.n, 256);
   const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * p.splits;
-  if (tiles > kMostItems / 512) return hipErrorInvalidValue;
-  large_kernel<T, L, BM><<<(unsigned)tiles, 512, 0, s>>>(p);
+  if (tiles > INT32_MAX) return hipErrorInvalidValue;   // larger than any memory
+  large_kernel<T, L, BM><<<grid_of(tiles), 512, 0, s>>>(p);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess && p.splits > 1 ? launch_join(p, s, join_kernel<T>) : e;
 }
@@ -846,9 +852,9 @@ template <class T, int L>
 hipError_t launch_layout(const ProductArgs& p, const ProductPlan& plan, hipStream_t s) {
   if constexpr (L == kForward)
     if (plan.shape == kFewRows) {
-      const unsigned groups = (unsigned)ceil_div(p.n, 16);
-      if (p.m <= 16) few_rows_kernel<T, 1><<<groups, 512, 0, s>>>(p);
-      else few_rows_kernel<T, 2><<<groups, 512, 0, s>>>(p);
+      const dim3 grid = grid_of(ceil_div(p.n, 16));
+      if (p.m <= 16) few_rows_kernel<T, 1><<<grid, 512, 0, s>>>(p);
+      else few_rows_kernel<T, 2><<<grid, 512, 0, s>>>(p);
       return hipGetLastError();
     }
   if constexpr (sizeof(T) == 2) {
@@ -869,9 +875,7 @@ hipError_t align_operands(const AlignArgs& first, const AlignArgs& second, hipSt
   if (first.dst != nullptr) pieces[0] = first.rows * (first.ld_dst / kVec<T>);
   if (second.dst != nullptr) pieces[1] = second.rows * (second.ld_dst / kVec<T>);
   if (pieces[0] + pieces[1] == 0) return hipSuccess;
-  const int64_t groups = ceil_div(pieces[0] + pieces[1], 256);
-  if (groups > kMostItems / 256) return hipErrorInvalidValue;
-  align_kernel<T><<<(unsigned)groups, 256, 0, s>>>(first, second, pieces[0]);
+  align_kernel<T><<<grid_of(ceil_div(pieces[0] + pieces[1], 256)), 256, 0, s>>>(first, second, pieces[0]);
   return hipGetLastError();
 }
 
@@ -899,7 +903,7 @@ hipError_t launch_pair(ProductArgs x, ProductArgs w, const ColumnSums& sums, hip
     groups[i] = (int64_t)both[i]->tiles_m * both[i]->tiles_n * both[i]->splits;
   }
   groups[2] = sums.out != nullptr ? ceil_div(sums.n, kSumColumns) : 0;
-  if (groups[0] + groups[1] + groups[2] > kMostItems / 512) return hipErrorInvalidValue;
+  // few: the tiles are up to 4 a compute unit, the sums' columns no more than the tiles' rows
   pair_kernel<T, S><<<(unsigned)(groups[0] + groups[1] + groups[2]), kTileThreads<S>, 0, s>>>(
       x, w, (unsigned)groups[0], (unsigned)groups[1], sums);
   hipError_t e = hipGetLastError();

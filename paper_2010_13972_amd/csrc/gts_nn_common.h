@@ -33,6 +33,17 @@ inline bool misaligned(const void* p, int64_t to) {
 
 __host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// The grid of `groups` workgroups (at least 1): work-items along one axis have to stay below
+// 2^32, so past 2^20 workgroups they go on along the second, where the last row may be
+// longer than what is left.
+inline dim3 grid_of(int64_t groups) {
+  const int64_t along = groups < (1 << 20) ? groups : 1 << 20;
+  return dim3((unsigned)along, (unsigned)ceil_div(groups, along));
+}
+
+// The workgroup's number in such a grid.
+__device__ __forceinline__ int64_t group_of_grid() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // A matrix argument: its row stride must hold its width, both below 2^31.
 struct Matrix {
   const char* name;

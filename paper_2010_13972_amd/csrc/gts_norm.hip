@@ -102,8 +102,7 @@ __global__ __launch_bounds__(kThreads<TPR>) void norm_kernel(const gts_norm_args
   __shared__ float lds[2][4][RowSum<TPR>::kWaves];
   RowSum<TPR> row_sum{lds};
   const int t = threadIdx.x % TPR;
-  const int64_t group = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-  const int64_t row = group * (kThreads<TPR> / TPR) + threadIdx.x / TPR;
+  const int64_t row = group_of_grid() * (kThreads<TPR> / TPR) + threadIdx.x / TPR;
   if (row >= a.rows) return;   // rows of a workgroup share no barrier, or there is one
   const int64_t c = (int64_t)t * V;
   int64_t left[NV];
@@ -471,9 +470,7 @@ extern "C" gts_status gts_norm_residual(const gts_norm_args* a, void* stream) {
     return check_launch(with_shape(a->width, kVec<T>, [&](auto tpr, auto nv) {
       constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
       if constexpr (TPR * NV * kVec<T> < 2 * GTS_NORM_MAX_WIDTH) {
-        // a launch's work-items along one axis stay below 2^32
-        const int64_t groups = ceil_div(a->rows, kThreads<TPR> / TPR), along = std::min<int64_t>(groups, 1 << 20);
-        const dim3 grid((unsigned)along, (unsigned)ceil_div(groups, along));
+        const dim3 grid = grid_of(ceil_div(a->rows, kThreads<TPR> / TPR));
         norm_kernel<T, TPR, NV><<<grid, kThreads<TPR>, 0, static_cast<hipStream_t>(stream)>>>(*a);
         return hipGetLastError();
       } else {
