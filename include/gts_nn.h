@@ -247,7 +247,7 @@ typedef struct gts_tensor {
  * gts_grad_clip -- out[0] = norm, the root of the sum of the squares of all
  * gradients; out[1] = min(1, max_norm / (norm + 1e-6)), or NaN if the norm is not finite.
  * grad_dtype: any of the three types.  d_out: device float[2].  Squares are summed in
- * 32 bits a workgroup and in 64 across workgroups, in a fixed order.
+ * 64 bits, in a fixed order.
  */
 gts_status gts_grad_clip_workspace_bytes(const gts_tensor *tensors, int64_t num_tensors,
                                          int64_t *bytes);

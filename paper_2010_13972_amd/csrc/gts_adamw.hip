@@ -37,12 +37,13 @@ __device__ __forceinline__ int find(const Table& tab, int64_t chunk) {
   return lo;
 }
 
-// The sum of the squares of one chunk of one gradient.  Bound by memory: 127 M values in bf16
+// The sum of the squares of one chunk of one gradient, in 64 bits: squares of gradients above
+// 1.8e19 or below 1e-23 are no 32-bit numbers, though the norm is one.  Bound by memory: 127 M values in bf16
 // take 81 us after a step (3.1 TB/s; the step leaves its results dirty in the last-level
 // cache), 4.3 M take 4.9.
 template <class G>
-__global__ __launch_bounds__(256) void square_kernel(const Table tab, float* part) {
-  __shared__ float join[4];
+__global__ __launch_bounds__(256) void square_kernel(const Table tab, double* part) {
+  __shared__ double join[4];
   const int k = find(tab, blockIdx.x);
   const G* g = static_cast<const G*>(tab.t[k].grad);
   const int64_t begin = (blockIdx.x - tab.first[k]) * kChunk, count = tab.t[k].count;
@@ -53,22 +54,23 @@ __global__ __launch_bounds__(256) void square_kernel(const Table tab, float* par
     const int64_t at = begin + ((int64_t)j * 256 + threadIdx.x) * kItems;
     load_vec<G, kItems>(d[j], g + at, count - at);
   }
-  float acc = 0.0f;
+  double acc = 0.0;
 #pragma unroll
   for (int j = 0; j < TURNS; ++j)
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) acc += d[j][i] * d[j][i];
-  acc = lane_sum<64>(acc);
+    for (int i = 0; i < kItems; ++i) acc += (double)d[j][i] * (double)d[j][i];
+#pragma unroll
+  for (int k = 1; k < 64; k *= 2) acc += __shfl_xor(acc, k, 64);
   if (threadIdx.x % 64 == 0) join[threadIdx.x / 64] = acc;
   __syncthreads();
   if (threadIdx.x == 0) part[blockIdx.x] = (join[0] + join[1]) + (join[2] + join[3]);
 }
 
-__global__ __launch_bounds__(1024) void clip_kernel(const float* part, int64_t parts,
+__global__ __launch_bounds__(1024) void clip_kernel(const double* part, int64_t parts,
                                                     float max_norm, float* out) {
   __shared__ double join[1024];
   double acc = 0.0;
-  for (int64_t i = threadIdx.x; i < parts; i += 1024) acc += (double)part[i];
+  for (int64_t i = threadIdx.x; i < parts; i += 1024) acc += part[i];
   join[threadIdx.x] = acc;
   __syncthreads();
   for (int d = 512; d > 0; d /= 2) {
@@ -263,6 +265,9 @@ int64_t all_chunks(const gts_tensor* t, int64_t n) {
   return c;
 }
 
+// The chunks' sums.
+int64_t clip_bytes(int64_t chunks) { return ceil_div(chunks * (int64_t)sizeof(double), 16) * 16; }
+
 }  // namespace
 }  // namespace nn
 }  // namespace gts
@@ -276,7 +281,7 @@ extern "C" gts_status gts_grad_clip_workspace_bytes(const gts_tensor* tensors, i
     return fail(GTS_EINVAL, "tensors must not be NULL, num_tensors not negative");
   for (int64_t i = 0; i < num_tensors; ++i)
     if (tensors[i].count < 0) return fail(GTS_EINVAL, "tensor %lld: negative count", (long long)i);
-  *bytes = nn::ceil_div(nn::all_chunks(tensors, num_tensors) * 4, 16) * 16;
+  *bytes = nn::clip_bytes(nn::all_chunks(tensors, num_tensors));
   return GTS_OK;
 }
 
@@ -293,10 +298,9 @@ extern "C" gts_status gts_grad_clip(const gts_tensor* tensors, int64_t num_tenso
   if (d_out == nullptr || misaligned(d_out, 4)) return fail(GTS_EINVAL, "d_out is NULL or misaligned");
   if (!(max_norm > 0.0f)) return fail(GTS_EINVAL, "max_norm must be above 0");
   const int64_t chunks = all_chunks(tensors, num_tensors);
-  if ((st = check_workspace(d_workspace, workspace_bytes, ceil_div(chunks * 4, 16) * 16)) != GTS_OK)
-    return st;
+  if ((st = check_workspace(d_workspace, workspace_bytes, clip_bytes(chunks))) != GTS_OK) return st;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  float* part = static_cast<float*>(d_workspace);
+  double* part = static_cast<double*>(d_workspace);
   hipError_t e = for_tables(tensors, num_tensors, [&](const Table& tab, int64_t n) {
     with_type(grad_dtype, [&](auto g) {
       square_kernel<decltype(g)><<<(unsigned)n, 256, 0, s>>>(tab, part);
@@ -305,7 +309,7 @@ extern "C" gts_status gts_grad_clip(const gts_tensor* tensors, int64_t num_tenso
     return hipGetLastError();
   });
   if (e == hipSuccess) {
-    clip_kernel<<<1, 1024, 0, s>>>(static_cast<const float*>(d_workspace), chunks, max_norm, d_out);
+    clip_kernel<<<1, 1024, 0, s>>>(static_cast<const double*>(d_workspace), chunks, max_norm, d_out);
     e = hipGetLastError();
   }
   return e == hipSuccess ? GTS_OK : fail(GTS_EDEVICE, "clip launch failed: %s", hipGetErrorString(e));
