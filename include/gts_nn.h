@@ -3,8 +3,8 @@
  * part of libgts.
  *
  * gts_shap gives exact SHAP values at a cost that grows with the ensemble.  A
- * program that needs values at a fixed small cost trains a residual network on
- * them and asks the network instead.  These are the device operators such a network
+ * program that needs approximate values of many rows at a cost that does not trains
+ * a residual network on them and asks the network instead.  These are the device operators such a network
  * is trained and served with:
  *
  *   gts_linear                  y = act(x W^T + b) + r
@@ -110,7 +110,8 @@ gts_status gts_linear_config(int64_t rows, int64_t inputs, int64_t outputs, int3
  * gts_linear_backward -- the gradients of gts_linear: with dz = dy act'(z),
  * dx = dz W, dw = dz^T x, db = the column sums of dz.  (The residual's gradient
  * is dy itself.)  In 16 bits, dz is rounded to the type before the products, as
- * the matrix units take it; db sums it unrounded.
+ * the matrix units take it, which adds to the gradients' error what the rounding of their
+ * own makes (in bf16 1.7e-3 becomes 2.3e-3); db sums it unrounded.
  *
  * dy   [rows][outputs]; pre [rows][outputs]: z of the forward pass; unused and may be
  *      NULL for GTS_ACT_NONE.
@@ -264,7 +265,8 @@ gts_status gts_grad_clip(const gts_tensor *tensors, int64_t num_tensors, int32_t
  *
  * with c = d_clip[1] as gts_grad_clip writes it, 1 if d_clip is NULL.  If c is NaN
  * (gradients that are not finite), the step changes nothing but the copies, which
- * are written from the unchanged parameters.
+ * are written from the unchanged parameters.  g^2 is a 32-bit number: zero for |g| below
+ * 3e-23, infinite above 1.8e19.
  *
  * state_bits 32: m and v are float buffers; m_scale, v_scale are unused.
  * state_bits 8:  m and v hold 8-bit floats (OCP e4m3) and m_scale, v_scale one float for

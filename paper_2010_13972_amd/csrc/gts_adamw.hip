@@ -12,7 +12,7 @@ namespace gts {
 namespace nn {
 namespace {
 
-constexpr int kTensors = 80;         // 3.6 KB of arguments
+constexpr int kTensors = 80;         // 3856 bytes of arguments
 constexpr int kItems = 8;            // consecutive elements a thread takes
 constexpr int64_t kChunk = 256 * kItems * 4;
 constexpr int64_t kMostChunks = (1 << 24) - 1;   // of a launch
@@ -38,9 +38,10 @@ __device__ __forceinline__ int find(const Table& tab, int64_t chunk) {
 }
 
 // The sum of the squares of one chunk of one gradient, in 64 bits: squares of gradients above
-// 1.8e19 or below 1e-23 are no 32-bit numbers, though the norm is one.  Bound by memory: 127 M values in bf16
-// take 81 us after a step (3.1 TB/s; the step leaves its results dirty in the last-level
-// cache), 4.3 M take 4.9.
+// 1.8e19 or below 1e-23 are no 32-bit numbers, though the norm is one.  Bound by
+// memory: 127 M values in bf16 take 50 us with clip_kernel (5.1 TB/s) where no pass before
+// left the last-level cache full of results yet to be written, and 81 where one did, a fill
+// of 0.5 GB as well as the optimizer's step; 4.3 M take 5.1.
 template <class G>
 __global__ __launch_bounds__(256) void square_kernel(const Table tab, double* part) {
   __shared__ double join[4];
@@ -144,7 +145,7 @@ __device__ __forceinline__ void store_codes(uint8_t* p, uint2 c, int64_t n) {
 }
 
 // Bound by memory: with 8-bit states, fp32 weights, a bf16 gradient and copy 16 bytes a
-// parameter, 127 M of which take 374 us (5.4 TB/s); with 32-bit states 28 bytes, 4.3 M of
+// parameter, 127 M of which take 374 to 380 us (5.4 TB/s); with 32-bit states 28 bytes, 4.3 M of
 // which take 23 (5.2 TB/s, partly from the last-level cache).
 template <class P, class G, int BITS>
 __global__ __launch_bounds__(256) void adamw_kernel(const Table tab, const Step s) {

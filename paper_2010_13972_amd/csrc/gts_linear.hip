@@ -33,8 +33,9 @@ constexpr int kTileM[6] = {256, 192, 128, 64, 64, 128}, kTileN[6] = {256, 256, 1
 // again (dw of 3714 x 2552 x 816 62 us, 39 in tiles of 128 x 128), the larger ones, which
 // read a row for more columns, little.
 // Splits pay for writing and joining their sums: a launch and the traffic.  Up to 32 rows,
-// W passes once through registers: 16 rows of 1024 to 4096 in bf16 4.1 against 5.9, 64 rows
-// 7.3 against 6.0.
+// W passes once through registers: 1024 to 4096 in bf16 takes 16 rows 3.9 and 32 rows 4.9 in a
+// graph, and 5.8 in tiles, as 33 rows do.  (The same with 64 rows, which is not built, took
+// 7.3 against 6.0.)
 ProductPlan plan_product(int64_t m, int64_t n, int64_t k, int64_t size, Layout layout, int64_t copied,
                          int broken) {
   struct Cost {
@@ -202,6 +203,11 @@ int64_t product_bytes(int64_t m, int64_t n, int64_t k, Layout layout, int64_t si
 // its end.  dz or sums may be null; rows of dz are ld_dz apart, a multiple of kVec, and
 // end in zeros.  Bound by memory: 10000 x 4096 in bf16 with GELU 50 us under a profiler
 // (246 MB, 4.9 TB/s).
+//
+// In 16 bits dz is rounded to the type, since the matrix cores take no more: the gradients of
+// 10000 x 1024 x 4096 in bf16 are 2.3e-3 off 64 bits, where their own rounding alone makes
+// 1.7e-3.  What the rounding leaves could go in as a second operand, but would take both
+// products once more, some 200 us beside the 253 of the call.  The sums are of dz unrounded.
 template <class T, int LPR>
 __global__ __launch_bounds__(256) void dz_kernel(const T* dy, int64_t ld_dy, const T* pre,
                                                  int64_t ld_pre, int64_t rows, int64_t n,

@@ -214,7 +214,8 @@ struct GradRow {
 //
 // Bound by memory: 10000 x 2048 in bf16 takes 73 us with column_sums_kernel (4.5 TB/s over
 // the same inputs), 10000 x 4096 129 (5.1); 1000 x 785 in fp32 by two rows a workgroup and
-// their exchanges, 13 us.  16-bit rows past 8192 columns spill (4000 x 16384 515 us, 2 TB/s).
+// their exchanges, 13 us.  Rows past 8192 columns spill registers, 300 to 470 bytes a lane
+// (4000 x 16384 505 us in bf16, 2.1 TB/s; 679 in fp32, 3.1).
 template <class T, int TPR, int NV, bool LAYER, bool AHEAD>
 __global__ __launch_bounds__(kGradThreads<TPR>) void norm_grad_kernel(const gts_norm_grad_args a,
                                                                       float* part) {

@@ -1,9 +1,11 @@
-"""An explainer network: SHAP values of a tree ensemble at a fixed cost.
+"""An explainer network: SHAP values of a tree ensemble, approximately, at a fixed cost.
 
 ``gts.shap`` is exact, and its cost grows with the ensemble.  An ``Explainer`` learns to
 give the same values: every training step draws rows, computes their exact values with
 ``gts.shap`` and fits a residual network to them with the operators of ``nn``.  Asked
-for a row it then runs the network alone.
+for rows it then runs the network alone.  That pays for many rows of a large ensemble:
+10 000 rows of the deep workload take it 0.24 ms and gts.shap 2.2, of the small covtype_med
+0.25 and 0.31.  A single row is faster exact (17 to 44 us) than from the network's graph (60).
 
     x -> W_in, silu -> u                                     u: the residual stream
     per block:  gate = h W_g^T,  f = gelu(h W_1^T) W_2^T     h: the normed stream
@@ -113,7 +115,7 @@ class Explainer:
             dh, g[f"w_1.{b}"], g[f"b_1.{b}"] = nn.linear_backward(dz, h, w[f"w_1.{b}"], pre=pre,
                                                                   act="gelu")
             dg, g[f"w_g.{b}"], g[f"b_g.{b}"] = nn.linear_backward(n["dgate"], h, w[f"w_g.{b}"])
-            dh = dh + dg
+            dh = dh + dg   # rounded to the type, as every gradient on the way is
         if du is not None:   # the first block reads the stream itself
             dh = dh + du
         _, g["w_in"], g["b_in"] = nn.linear_backward(dh, x, w["w_in"], pre=pre_in, act="silu",
